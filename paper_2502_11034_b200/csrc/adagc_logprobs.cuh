@@ -96,6 +96,10 @@ __device__ __forceinline__ void copy_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
 }
 
+// Below this a logit's gradient is 0 where |lse| < 1024 (kExtremeLse): p = 2^d with d < -4400.  The gradient's kernel raises smaller
+// logits (masked ones) to it, so that d stays small enough for B d to be finite: A + B d with p = 0 has to give 0.
+constexpr float kLowestLogit = -4096.0f;
+
 template <bool kBF16>
 struct Elem;  // 16-byte vectors of the logits' type
 template <>
@@ -122,10 +126,10 @@ struct Elem<true> {
       if (i < n) m = __hmax2(__hmax2(m, __hmax2(pair(w[i].x), pair(w[i].y))), __hmax2(pair(w[i].z), pair(w[i].w)));
     return fmaxf(__low2float(m), __high2float(m));
   }
-  static __device__ __forceinline__ uint4 clamped(uint4 w) {  // at least -1e38; a NaN stays
+  static __device__ __forceinline__ uint4 clamped(uint4 w) {  // at least kLowestLogit; a NaN stays
     uint32_t* u = &w.x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u[i]) : "r"(0xfe96fe96u));
+    for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u[i]) : "r"(0xc580c580u));
     return w;
   }
   static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
@@ -145,7 +149,7 @@ struct Elem<false> {
   static __device__ __forceinline__ uint4 clamped(uint4 w) {
     uint32_t* u = &w.x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+r"(u[i]) : "r"(0xfe967699u));
+    for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+r"(u[i]) : "r"(0xc5800000u));
     return w;
   }
   template <int kN>
@@ -642,6 +646,7 @@ struct RowGrad {
   bool extreme;  // lse rounded to fp32 has lost too much of ln s
 };
 constexpr float kExtremeLse = 1024.0f;  // beyond this an fp32 lse is off by 2^-15 or more, and every p by that factor
+static_assert((kLowestLogit + kExtremeLse) * kLog2e < -200.0f, "p of the lowest logit is 0");
 __device__ __forceinline__ RowGrad row_grad(const RowInputs& i, int vocab) {
   RowGrad g;
   const bool wild = i.target >= vocab;
@@ -655,8 +660,8 @@ __device__ __forceinline__ RowGrad row_grad(const RowInputs& i, int vocab) {
   if (wild && g.a != 0.0f) g.A = quiet_nan();
   return g;
 }
-// Two entries, clamped beforehand to at least -1e38 (-inf * 0 is a NaN); NaN entries stay.  fp32 gradients keep
-// probabilities below 2^-126, for which the exponential costs more instructions.
+// Two entries, clamped beforehand to at least kLowestLogit (so |d| < 7400 where p = 0, and B d is finite for any |c| < 6e34); NaN
+// entries stay.  fp32 gradients keep probabilities below 2^-126, for which the exponential costs more instructions.
 template <bool kBF16>
 __device__ __forceinline__ void grad_pair(float& z0, float& z1, const RowGrad& g) {
   const uint64_t d = mul2(add2(pack2(z0, z1), pack2(-g.lse, -g.lse)), pack2(kLog2e, kLog2e));
@@ -667,7 +672,7 @@ __device__ __forceinline__ void grad_pair(float& z0, float& z1, const RowGrad& g
 }
 template <bool kBF16>
 __device__ __forceinline__ float grad_one(float z, const RowGrad& g) {
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(z) : "f"(-1e38f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(z) : "f"(kLowestLogit));
   float z1 = 0.0f;
   grad_pair<kBF16>(z, z1, g);
   return z;
