@@ -54,11 +54,11 @@ int adagc_token_logprobs(const void* d_logits, int32_t logits_dtype, int64_t row
  *   d_grad_logprob, d_grad_lse, d_grad_entropy   rows fp32 each; NULL means zero.  d_targets is needed with d_grad_logprob.
  *   d_grad_logits  [rows, vocab] in logits_dtype, leading dimension grad_ld.  It may be d_logits itself (same pointer and
  *                  ld: in place); any other overlap is ADAGC_E_OVERLAP.
- * Masked entries get 0 and so does a row with every entry masked.  A row without a target ignores a.  A row whose three
- * upstream gradients are zero (or absent) gets zeros whatever its logits hold; they are not read.  A target >= vocab with
- * a != 0 gives a row of NaN.  ln p_j is formed as z_j - lse, so it shares the rounding of the fp32 lse; rows with
- * |lse| >= 1024, where that would matter (up to rows whose entries are all the type's lowest value), take their sum anew
- * from the logits.
+ * Masked entries get 0 (a target that is masked itself, whose logprob is -inf, gets a) and so does a row with every entry
+ * masked.  A row without a target ignores a.  A row whose three upstream gradients are zero (or absent) gets zeros whatever
+ * its logits hold; they are not read.  A target >= vocab with a != 0 gives a row of NaN.  ln p_j is formed as z_j - lse, so it
+ * shares the rounding of the fp32 lse; rows with |lse| >= 1024, where that would matter (up to rows whose entries are all the
+ * type's lowest value), take their sum anew from the logits.
  */
 int adagc_token_logprobs_backward(const void* d_logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t ld,
                                   const int64_t* d_targets, const float* d_lse, const float* d_entropy,

@@ -717,9 +717,10 @@ adagc_token_logprobs_grad_kernel(LogprobGradArgs x) {
       }
       const float shift = log2f(p.s);
       for (int j = tid; j < x.vocab; j += kT) {
-        const float d = fmaf(E::load(in, j) - p.m, kLog2e, -shift);
-        const float e = exp2_full(d);
-        E::store(out, j, (e == 0.0f ? 0.0f : e * fmaf(g.B, d, g.A)) + (j == g.target ? g.a : 0.0f));
+        float d = fmaf(E::load(in, j) - p.m, kLog2e, -shift);
+        // p is 0 from there on, and B d stays finite; a NaN, of the row or of A, passes
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(d) : "f"(kExpFloor));
+        E::store(out, j, exp2_full(d) * fmaf(g.B, d, g.A) + (j == g.target ? g.a : 0.0f));
       }
       continue;
     }

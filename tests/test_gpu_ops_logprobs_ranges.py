@@ -1,4 +1,5 @@
-"""Gradient of the token log probabilities at the ends of its range.
+"""Gradient of the token log probabilities at the ends of its range: large upstream gradients over masked entries, targets that are
+masked, and targets outside the vocabulary in rows of extreme magnitudes.
 
 Masked entries: p = 0, so the gradient is 0 exactly, however large the upstream gradients are; the other entries have the tolerance
 of test_gpu_ops_logprobs.check_backward."""
@@ -44,3 +45,37 @@ def test_masked_entries_get_zero_whatever_flows_into_the_entropy(dtype, vocab, s
         logprobs.token_logprobs_backward(z, t, r.lse, r.entropy, a, b, cv, out=out)
         assert (out[hidden] == 0).all()
         check_backward(z, t, r.lse, r.entropy, a, b, cv, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [50, 9001])
+def test_target_outside_the_vocabulary_in_rows_of_extreme_magnitude(dtype, vocab):
+    """The row is NaN throughout, also where p is 0."""
+    gen = torch.Generator("cuda").manual_seed(vocab)
+    z = (torch.randn(5, vocab, device="cuda", generator=gen) * 3 + 4096).to(DT[dtype])
+    z[1, ::2] = NINF
+    z[2, ::2] = torch.finfo(DT[dtype]).min
+    z[3] = torch.finfo(DT[dtype]).min
+    z[4, 1:] -= 3000
+    t = torch.tensor([vocab, vocab + 7, vocab, vocab, vocab], device="cuda")
+    r = logprobs.token_logprobs(z, t)
+    assert (r.lse.abs() >= 1024).all()
+    a = torch.full((5,), 0.5, device="cuda")
+    got = logprobs.token_logprobs_backward(z, t, r.lse, r.entropy, a, a, a)
+    assert torch.isnan(got).all()
+    got = logprobs.token_logprobs_backward(z, t, r.lse, r.entropy, None, a, a)      # the target plays no part
+    check_backward(z, t, r.lse, r.entropy, None, a, a, got)
+
+
+def test_masked_target():
+    """logprob = -inf; its gradient at the target is the upstream one (p = 0 there), the other masked entries get 0."""
+    z = torch.randn(2, 300, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    z[:, 100:200] = NINF
+    t = torch.tensor([150, 20], device="cuda")
+    r = logprobs.token_logprobs(z, t)
+    a = torch.tensor([0.25, -0.5], device="cuda")
+    g = logprobs.token_logprobs_backward(z, t, r.lse, grad_logprob=a)
+    assert float(r.logprob[0]) == NINF and float(g[0, 150]) == 0.25
+    g[0, 150] = 0
+    assert (g[:, 100:200] == 0).all()
+    check_backward(z, t, r.lse, r.entropy, a, None, None, logprobs.token_logprobs_backward(z, t, r.lse, grad_logprob=a))
