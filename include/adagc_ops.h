@@ -56,9 +56,10 @@ int adagc_token_logprobs(const void* d_logits, int32_t logits_dtype, int64_t row
  *                  ld: in place); any other overlap is ADAGC_E_OVERLAP.
  * Masked entries get 0 (a target that is masked itself, whose logprob is -inf, gets a) and so does a row with every entry
  * masked.  A row without a target ignores a.  A row whose three upstream gradients are zero (or absent) gets zeros whatever
- * its logits hold; they are not read.  A target >= vocab with a != 0 gives a row of NaN.  ln p_j is formed as z_j - lse, so it
- * shares the rounding of the fp32 lse; rows with |lse| >= 1024, where that would matter (up to rows whose entries are all the
- * type's lowest value), take their sum anew from the logits.
+ * its logits hold; they are not read.  A target >= vocab with a != 0 gives a row of NaN.  ln p_j is formed as z_j - lse, so
+ * every p of a row shares the rounding of its fp32 lse, a relative error of |lse| 2^-24 at most (3e-5 where |lse| is from 512
+ * to 1024).  Rows with |lse| >= 1024, where it would be larger (up to rows whose entries are all the type's lowest value),
+ * take their sum anew from the logits, at the cost of a second pass.
  */
 int adagc_token_logprobs_backward(const void* d_logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t ld,
                                   const int64_t* d_targets, const float* d_lse, const float* d_entropy,

@@ -645,7 +645,9 @@ struct RowGrad {
   bool zero;     // nothing flows into this row
   bool extreme;  // lse rounded to fp32 has lost too much of ln s
 };
-constexpr float kExtremeLse = 1024.0f;  // beyond this an fp32 lse is off by 2^-15 or more, and every p by that factor
+// An lse rounded to fp32 is off by half an ulp at most: 2^-15 from 512 on, 2^-14 from 1024 on, and so on, and every p of the row by
+// that factor.  From here on the row's sum is taken anew.
+constexpr float kExtremeLse = 1024.0f;
 static_assert((kLowestLogit + kExtremeLse) * kLog2e < -200.0f, "p of the lowest logit is 0");
 __device__ __forceinline__ RowGrad row_grad(const RowInputs& i, int vocab) {
   RowGrad g;

@@ -1,11 +1,16 @@
-"""Gradient of the token log probabilities at the ends of its range: large upstream gradients over masked entries, targets that are
-masked, and targets outside the vocabulary in rows of extreme magnitudes.
+"""Gradient of the token log probabilities at the ends of its range: large upstream gradients over masked entries, targets that are masked,
+targets outside the vocabulary in rows of extreme magnitudes, and rows far from zero.
 
 Masked entries: p = 0, so the gradient is 0 exactly, however large the upstream gradients are; the other entries have the tolerance
-of test_gpu_ops_logprobs.check_backward."""
+of test_gpu_ops_logprobs.check_backward.  Shifted rows are compared end to end, with the row's own float64 lse: the kernel's lse is off
+by 2e-5 plus one rounding to fp32, half an ulp, which enters the exponent of every p; rows of |lse| >= 1024 take their sum anew and do
+not have the half ulp."""
+import math
+
 import pytest
 import torch
 
+import ops_reference as R
 from paper_2502_11034_b200 import logprobs
 from test_gpu_ops_logprobs import DT, NINF, check_backward, strided
 
@@ -79,3 +84,29 @@ def test_masked_target():
     g[0, 150] = 0
     assert (g[:, 100:200] == 0).all()
     check_backward(z, t, r.lse, r.entropy, a, None, None, logprobs.token_logprobs_backward(z, t, r.lse, grad_logprob=a))
+
+
+@pytest.mark.parametrize("shift", [0, 100, 500, 1000, 1015, 1100, 5000, -1000, -5000])
+def test_gradient_of_shifted_rows_end_to_end(shift):
+    gen = torch.Generator("cuda").manual_seed(abs(shift))
+    rows, vocab = 3, 2000
+    z = torch.randn(rows, vocab, device="cuda", generator=gen) * 3 + shift
+    t = torch.randint(0, vocab, (rows,), device="cuda", generator=gen)
+    a, b, c = (torch.randn(rows, device="cuda", generator=gen) for _ in range(3))
+    r = logprobs.token_logprobs(z, t)
+    got = logprobs.token_logprobs_backward(z, t, r.lse, r.entropy, a, b, c).double().cpu()
+    zd = z.double().cpu()
+    zd0 = zd - shift                                           # exact in float64; the gradient does not depend on the shift
+    exact = R.logprobs(zd0, t.cpu())
+    av, bv, cv = (v.double().cpu()[:, None] for v in (a, b, c))
+    want = R.logprobs_grad(zd0, t.cpu(), exact["lse"], exact["entropy"], av[:, 0], bv[:, 0], cv[:, 0])
+    d = torch.log_softmax(zd0, -1)
+    h = exact["entropy"][:, None]
+    lse = exact["lse"][:, None] + shift
+    half_ulp = torch.where(lse.abs() < 1024, torch.exp2(torch.floor(torch.log2(lse.abs())) - 24), torch.zeros_like(lse))
+    off = 2e-5 + half_ulp
+    bracket = av.abs() + bv.abs() + cv.abs() * (h + d.abs())
+    tol = torch.exp(d) * (bracket * (2 ** -21 + d.abs() * 2 ** -22 + off) + cv.abs() * (off + 2e-5 * (1 + h))) + 1e-37
+    tol.scatter_add_(1, t.cpu()[:, None], av.abs() * 2 ** -22)
+    worst = float(((got - want).abs() / tol).max())
+    assert worst <= 1 and not math.isnan(worst), worst
