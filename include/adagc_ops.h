@@ -98,6 +98,8 @@ int adagc_act8_decode(const adagc_act8* in, int64_t rows, int64_t cols, void* d_
  * Gated activation of a SwiGLU MLP, keeping its inputs in 8 bits for the backward pass:
  *     h = silu(gate) * up,  silu(x) = x / (1 + exp(-x)),  from the inputs as given;   *gate8 = act8(gate), *up8 = act8(up)
  * gate, up, h: [rows, cols] in dtype, each with its own leading dimension.
+ * fp32: h is within 2^-21 of its value (relative) where 1 / (1 + exp(-gate)) is a normal number.  bf16: exp is taken with a
+ * relative error of about |gate| 2^-24, far below the rounding of h.  The backward pass likewise.
  */
 int adagc_act8_swiglu(const void* d_gate, int64_t ld_gate, const void* d_up, int64_t ld_up, int32_t dtype, int64_t rows,
                       int64_t cols, void* d_h, int64_t ld_h, const adagc_act8* gate8, const adagc_act8* up8,

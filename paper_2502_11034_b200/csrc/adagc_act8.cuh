@@ -292,7 +292,13 @@ __device__ __forceinline__ void decode_unit(const EncodedUnit& e, float (&v)[kUn
   }
 }
 
+// 1 / (1 + e^-x).  For bfloat16 results the exponential is one multiplication and one instruction: its relative error grows as
+// |x| 2^-24 (4e-6 at -80), a thousandth of their rounding.  fp32 results take the accurate exponential and reciprocal.  Measured
+// approximate / accurate, gated activation of 8192 x 11008: bf16 110 / 131 us forward, 135 / 150 us backward with h; fp32 189 / 189
+// and 201 / 202 us (HBM), and 57 / 62 and 81 / 88 us for 2731 columns.
+template <bool kBF16>
 __device__ __forceinline__ float sigmoid(float x) {
+  if constexpr (!kBF16) return __frcp_rn(1.0f + expf(-x));
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + exp2_approx(-kLog2e * x)));
   return r;
@@ -372,7 +378,7 @@ adagc_act8_swiglu_kernel(MatrixIn gate, MatrixIn up, MatrixOut h, CheckpointPtrs
     }
     float y[kUnit];
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) y[j] = a[u][j] * sigmoid(a[u][j]) * b[u][j];
+    for (int j = 0; j < kUnit; ++j) y[j] = a[u][j] * sigmoid<kBF16>(a[u][j]) * b[u][j];
     store_unit<kBF16, kRows>(h, p, g.cols, y, warp_stage<kBF16, kRows>());
   }
 }
@@ -401,7 +407,7 @@ adagc_act8_swiglu_grad_kernel(MatrixIn grad_h, CheckpointPtrs gate8, CheckpointP
     decode_unit(eb[u], b);
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) {
-      const float s = sigmoid(a[j]), as = a[j] * s;
+      const float s = sigmoid<kBF16>(a[j]), as = a[j] * s;
       h[j] = as * b[j];
       b[j] = dh[u][j] * b[j] * s * fmaf(a[j], 1.0f - s, 1.0f);
       a[j] = dh[u][j] * as;
