@@ -119,7 +119,7 @@ __device__ __forceinline__ void load_unit(const MatrixIn& a, const UnitPlace<kRo
       if (done) {
         alignas(16) uint32_t x[4 * kVectors + 4];
 #pragma unroll
-        for (int i = 0; i <= kVectors; ++i) reinterpret_cast<uint4*>(x)[i] = __ldg(reinterpret_cast<const uint4*>(from) + i);
+        for (int i = 0; i <= kVectors; ++i) reinterpret_cast<uint4*>(x)[i] = reinterpret_cast<const uint4*>(from)[i];  // (an ordinary load: see ld_once)
         shift_words<kBF16>(x, off, w);
       }
     }

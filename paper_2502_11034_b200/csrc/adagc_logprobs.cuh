@@ -81,9 +81,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-__device__ __forceinline__ uint4 ld_once(const uint4* p) {  // read once: no room in L1
+// Read once: no room in L1.  Not through the read-only path: a kernel may be started while the one that writes its inputs still runs
+// (griddep_wait comes before the first load), so they are not read-only for as long as it lives.
+__device__ __forceinline__ uint4 ld_once(const uint4* p) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
 }
 
