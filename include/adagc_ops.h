@@ -121,7 +121,8 @@ int adagc_act8_swiglu_backward(const void* d_grad_h, int64_t ld_grad_h, int32_t 
  *   d_grad_y       [tokens, out_features] bfloat16 (grad_y_dtype must be ADAGC_BF16), leading dimension ld_grad_y
  *   x8             checkpoint of [tokens, in_features]
  *   d_grad_w       [out_features, in_features] in grad_w_dtype, leading dimension ld_grad_w: a tensor of the gradient arena
- *   accumulate     0: overwrite; 1: add to what d_grad_w holds (read in its dtype, added in fp32, rounded once)
+ *   accumulate     0: overwrite; 1: add to what d_grad_w holds (the finished sum is added to it in fp32 and rounded once; fp32
+ *                  results below 2^-126 may become 0)
  *   d_workspace    adagc_act8_linear_wgrad_workspace_bytes(...) bytes, 256-byte aligned; its content is not kept
  * tokens = 0 gives dW = 0 (or leaves d_grad_w alone with accumulate).
  * The kernels wait on shared-memory barriers with a time limit of 2 s; a block that gives up writes NaN over its tile of

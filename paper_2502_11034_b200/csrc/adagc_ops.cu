@@ -227,7 +227,7 @@ bool make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int6
 struct WgradPlan {
   int tiles_n, steps, whole, tail, splits, steps_per_split;
   int64_t pitch;  // of the packed dY in elements, 0: dY is read in place
-  int64_t pack_bytes, bytes;
+  int64_t pack_bytes, bytes;  // the packed dY, then partial sums: of split tiles, then one block for each pair
 };
 constexpr int kB200Pairs = 74;  // plans do not depend on the device present: the workspace is sized without one
 WgradPlan wgrad_plan(int64_t tokens, int64_t n, int64_t k, const void* dy, int64_t ld) {
@@ -250,7 +250,8 @@ WgradPlan wgrad_plan(int64_t tokens, int64_t n, int64_t k, const void* dy, int64
   p.whole = tiles - p.tail;
   p.pitch = on_boundary(dy, 16) && ld % 8 == 0 && ld < (int64_t{1} << 38) ? 0 : (n + 7) / 8 * 8;
   p.pack_bytes = (tokens * p.pitch * 2 + 255) / 256 * 256;
-  p.bytes = p.pack_bytes + static_cast<int64_t>(p.splits) * p.tail * kWgTileN * kWgPairK * 4;
+  constexpr int64_t tile_bytes = int64_t{kWgTileN} * kWgPairK * 4;
+  p.bytes = p.pack_bytes + (p.splits * p.tail + (p.steps > kWgExactSteps ? std::min(p.whole, kB200Pairs) : 0)) * tile_bytes;
   return p;
 }
 bool valid_wgrad(int64_t tokens, int64_t n, int64_t k, int64_t ld) {
@@ -467,7 +468,6 @@ int adagc_act8_linear_wgrad(const void* d_grad_y, int32_t grad_y_dtype, int64_t 
   if (sms == 0) return ADAGC_E_CUDA;
 
   const void* dy = p.pitch ? d_workspace : d_grad_y;
-  float* partials = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.pack_bytes);
   CUtensorMap map_codes, map_dy;
   if (!make_map(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, x8->codes, pitch, tokens, pitch, kWgTileK, kWgStep) ||
       !make_map(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, n, tokens, (p.pitch ? p.pitch : ld_grad_y) * 2, 64, kWgStep))
@@ -486,7 +486,7 @@ int adagc_act8_linear_wgrad(const void* d_grad_y, int32_t grad_y_dtype, int64_t 
   a.exps = x8->exps;
   a.exps_pitch = pitch / kGroup;
   a.out = d_grad_w;
-  a.partials = partials;
+  a.partials = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.pack_bytes);
   a.ld_out = ld_grad_w;
   a.tokens = static_cast<int>(tokens);
   a.n = static_cast<int>(n);
@@ -499,10 +499,11 @@ int adagc_act8_linear_wgrad(const void* d_grad_y, int32_t grad_y_dtype, int64_t 
   a.steps_per_split = p.steps_per_split;
   const int flushes = bf16 ? 1 : (p.steps + kWgExactSteps - 1) / kWgExactSteps;
   a.steps_per_flush = (p.steps + flushes - 1) / flushes;
+  a.apart = accumulate && !bf16 && flushes > 1;
   a.out_bf16 = bf16;
   a.accumulate = accumulate;
-  const int units = p.whole + p.tail * p.splits;
-  if (int rc = launch(adagc_act8_wgrad_kernel, 2 * std::min(units, sms / 2), kWgThreads, kWgSmem, 1, s, map_codes, map_dy, a)) return rc;
+  const int pairs = std::min({p.whole + p.tail * p.splits, sms / 2, kB200Pairs});
+  if (int rc = launch(adagc_act8_wgrad_kernel, 2 * pairs, kWgThreads, kWgSmem, 1, s, map_codes, map_dy, a)) return rc;
   if (!p.tail) return ADAGC_OK;
   return launch(bf16 ? adagc_act8_wgrad_join_kernel<true> : adagc_act8_wgrad_join_kernel<false>, p.tail * kWgTileN, kWgPairK, 0, 1, s, a);
 }

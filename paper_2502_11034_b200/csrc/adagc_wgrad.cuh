@@ -24,7 +24,9 @@
 // The tensor core cuts, not rounds, when it adds to an accumulator: measured against 64 bits, the relative error of a
 // gradient grows from 2e-7 (1024 tokens) over 1.1e-6 (4096) to 7e-6 (16384), and twice that where the tokens' scales differ.
 // An fp32 result therefore leaves the accumulator every 1536 tokens at most and is added up in fp32 with rounding; a bf16
-// result does not need that (8192 x 4096 x 11008, fp32 out: 567 us with 2816, 664 with 1536, 728 with 1024).
+// result does not need that (8192 x 4096 x 11008, fp32 out: 567 us with 2816, 664 with 1536, 728 with 1024).  It is added up in
+// dW itself, or, if dW holds something to be added to, in a block of the workspace (750 to 790 us; adding each time to dW took 760
+// to 790 and rounded as often): the old values may be far above the sum, and are rounded onto once.
 #pragma once
 
 #include <cuda.h>
@@ -51,7 +53,7 @@ constexpr uint32_t kWgInstr = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | 
 struct WgradArgs {
   const uint8_t* exps;
   void* out;        // dW
-  float* partials;  // of the split tiles: one 256 x 256 block (n, k) per split and tile
+  float* partials;  // 256 x 256 blocks (n, k): of the split tiles, one per split and tile; then, with `apart`, one per pair
   int64_t ld_out, exps_pitch;
   int tokens, n, k;
   int tiles_n;
@@ -59,6 +61,7 @@ struct WgradArgs {
   int steps, steps_per_split;  // of kWgStep tokens
   int steps_per_flush;
   int out_bf16, accumulate;
+  int apart;  // tiles taken whole are summed up in their pair's block and added to dW at their end
 };
 
 constexpr uint64_t kDrainNs = 100000000ull;  // for what is still in flight when a block gives up
@@ -151,13 +154,15 @@ struct WgTile {
 };
 struct WgUnit {  // one tile of dW over one range of steps
   int n0, k0, step0, steps;
-  int block;  // of the partials, -1: the tile is taken whole
+  int block;  // of the partials, -1: into dW
+  bool whole;
   __device__ __forceinline__ WgUnit(const WgradArgs& a, int u, int rank) {
     const int split = u < a.whole ? 0 : (u - a.whole) / a.tail, tile = u < a.whole ? u : a.whole + (u - a.whole) % a.tail;
     const WgTile t(a.tiles_n, tile);
     n0 = t.n0;
     k0 = t.k0 + rank * kWgTileK;
-    block = u < a.whole ? -1 : u - a.whole;
+    whole = u < a.whole;
+    block = !whole ? u - a.whole : a.apart ? a.tail * a.splits + static_cast<int>(blockIdx.x / 2) : -1;
     step0 = split * a.steps_per_split;
     steps = u < a.whole ? a.steps : min(a.steps_per_split, a.steps - step0);
   }
@@ -167,6 +172,7 @@ __device__ __forceinline__ float wg_load(const float* p) { return *p; }
 __device__ __forceinline__ float wg_load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void wg_put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void wg_put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void wg_add(float* p, float x) { asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x) : "memory"); }
 
 // One lane's row of an accumulator (one k, 256 n) into `out`, n by n `ld` apart; with kAdd, onto what is there, whose loads
 // run 32 ahead (the first ones while the MMAs still run).  The accumulator is read 16 columns ahead of the stores.  !ok: NaN.
@@ -219,7 +225,29 @@ __device__ __forceinline__ void wg_store(T* out, int64_t ld, int n, bool mine, u
   }
 }
 
-// Calls flush(unit, first step, steps, first flush of the unit) for everything this pair of blocks has to do, in order;
+// The end of a tile that is summed up apart from dW: the accumulator and `sums`, added, onto what `out` holds, in one rounding (one
+// addition per element: nothing depends on an order).  A reduction in place of a load and a store, because the usual paths leave no
+// registers for both: with loads here 8192 x 4096 x 11008 took 950 to 1280 us instead of 760.
+template <typename Arrived>
+__device__ __forceinline__ void wg_finish(float* out, int64_t ld, const float* sums, int n, uint32_t acc, const bool& ok, Arrived arrived) {
+  constexpr int kCols = 16;
+  arrived();
+#pragma unroll 1
+  for (int c0 = 0; c0 < kWgTileN; c0 += kCols, sums += kCols * kWgPairK) {
+    float sum[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) sum[c] = sums[c * kWgPairK];
+    uint32_t v[kCols];
+    __syncwarp();
+    wg_tmem_load16(acc + c0, v);
+    wg_tmem_wait(v);
+#pragma unroll
+    for (int c = 0; c < kCols; ++c, out += ld)
+      if (c0 + c < n) wg_add(out, ok ? __uint_as_float(v[c]) + sum[c] : quiet_nan());
+  }
+}
+
+// Calls flush(unit, first step, steps, first flush of the unit, last one) for everything this pair of blocks has to do, in order;
 // every role goes through the same list.
 template <typename F>
 __device__ __forceinline__ void wg_each(const WgradArgs& a, int rank, F flush) {
@@ -227,7 +255,7 @@ __device__ __forceinline__ void wg_each(const WgradArgs& a, int rank, F flush) {
   for (int u = blockIdx.x / 2; u < units; u += gridDim.x / 2) {
     const WgUnit w(a, u, rank);
     for (int i = 0; i < w.steps; i += a.steps_per_flush)
-      if (!flush(w, w.step0 + i, min(a.steps_per_flush, w.steps - i), i == 0)) return;
+      if (!flush(w, w.step0 + i, min(a.steps_per_flush, w.steps - i), i == 0, i + a.steps_per_flush >= w.steps)) return;
   }
 }
 
@@ -284,7 +312,7 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
     if (lane == 0) {
       int it = 0;
       bool ok = true;
-      wg_each(a, rank, [&](const WgUnit& w, int step0, int steps, bool) {
+      wg_each(a, rank, [&](const WgUnit& w, int step0, int steps, bool, bool) {
         for (int i = 0; i < steps; ++i, ++it) {
           const int s = it % kWgSlotsCodes;
           if (it >= kWgSlotsCodes && !(ok = wg_wait(&free_codes[s], (it / kWgSlotsCodes - 1) & 1, gave_up))) return false;
@@ -302,7 +330,7 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
       int tile = 0, s = 0, parity = 0;
       bool ok = true, there = false;
       const uint64_t desc_a = wg_smem_desc(smem_u32(tile_a), kWgAtom), desc_b = wg_smem_desc(smem_u32(tile_b), kWgAtom);
-      wg_each(a, rank, [&](const WgUnit&, int, int steps, bool) {
+      wg_each(a, rank, [&](const WgUnit&, int, int steps, bool, bool) {
         const int buf = tile & 1;
         if (tile >= 2 && !(ok = __all_sync(0xffffffffu, wg_wait(&acc_empty[buf], (tile / 2 - 1) & 1, gave_up)))) return false;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -332,7 +360,7 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
     }
   } else if (warp == 2) {  // exponents: four bytes per token and step, two tokens per lane
     int it = 0;
-    wg_each(a, rank, [&](const WgUnit& w, int step0, int steps, bool) {
+    wg_each(a, rank, [&](const WgUnit& w, int step0, int steps, bool, bool) {
       for (int i = 0; i < steps; ++i, ++it) {
         const int s = it % kWgSlotsCodes;
         if (it >= kWgSlotsCodes && !wg_wait(&free_codes[s], (it / kWgSlotsCodes - 1) & 1, gave_up)) return false;
@@ -354,7 +382,7 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
     if (lane == 0) {
       int it = 0;
       bool ok = true;
-      wg_each(a, rank, [&](const WgUnit& w, int step0, int steps, bool) {
+      wg_each(a, rank, [&](const WgUnit& w, int step0, int steps, bool, bool) {
         for (int i = 0; i < steps; ++i, ++it) {
           const int s = it % kWgSlots;
           if (it >= kWgSlots && !(ok = wg_wait(&free_ab[s], (it / kWgSlots - 1) & 1, gave_up))) return false;
@@ -375,7 +403,7 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
     const int r0 = t >> 2, q = t & 3;  // first token of the step (then every kRows-th), group of 32 features
     const int flip = q >> 1;  // the two upper groups go through their halves in the other order: no bank conflicts
     int it = 0;
-    wg_each(a, rank, [&](const WgUnit&, int, int steps, bool) {
+    wg_each(a, rank, [&](const WgUnit&, int, int steps, bool, bool) {
       for (int i = (team - it % kWgDecodeTeams + kWgDecodeTeams) % kWgDecodeTeams; i < steps; i += kWgDecodeTeams) {
         const int x = it + i, sc = x % kWgSlotsCodes, sa = x % kWgSlots;
         bool ok = wg_wait(&full_codes[sc], (x / kWgSlotsCodes) & 1, gave_up);
@@ -411,7 +439,7 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
     const int quad = warp & 3;
     int tile = 0;
     bool ok = true;
-    wg_each(a, rank, [&](const WgUnit& w, int, int, bool first) {
+    wg_each(a, rank, [&](const WgUnit& w, int, int, bool first, bool last) {
       const int buf = tile & 1, k = w.k0 + quad * 32 + lane;
       const uint32_t acc = tmem + (static_cast<uint32_t>(quad * 32) << 16) + buf * kWgTileN;
       const auto arrived = [&] {
@@ -419,7 +447,10 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       };
       const bool part = w.block >= 0, add = !first || (a.accumulate && !part);
-      if (part || !a.out_bf16) {
+      if (part && w.whole && last) {
+        wg_finish(static_cast<float*>(a.out) + w.n0 * a.ld_out + k, a.ld_out,
+                  a.partials + static_cast<int64_t>(w.block) * kWgTileN * kWgPairK + (rank * kWgTileK + quad * 32 + lane), k < a.k ? a.n - w.n0 : 0, acc, ok, arrived);
+      } else if (part || !a.out_bf16) {
         float* out = part ? a.partials + static_cast<int64_t>(w.block) * kWgTileN * kWgPairK + (rank * kWgTileK + quad * 32 + lane)
                           : static_cast<float*>(a.out) + w.n0 * a.ld_out + k;
         const int64_t ld = part ? kWgPairK : a.ld_out;
