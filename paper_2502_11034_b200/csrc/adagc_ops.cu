@@ -497,9 +497,9 @@ int adagc_act8_linear_wgrad(const void* d_grad_y, int32_t grad_y_dtype, int64_t 
   a.splits = p.splits;
   a.steps = p.steps;
   a.steps_per_split = p.steps_per_split;
-  const int flushes = bf16 ? 1 : (p.steps + kWgExactSteps - 1) / kWgExactSteps;
+  const int most = bf16 ? kWgLongSteps : kWgExactSteps, flushes = (p.steps + most - 1) / most;
   a.steps_per_flush = (p.steps + flushes - 1) / flushes;
-  a.apart = accumulate && !bf16 && flushes > 1;
+  a.apart = (accumulate || bf16) && flushes > 1;
   a.out_bf16 = bf16;
   a.accumulate = accumulate;
   const int pairs = std::min({p.whole + p.tail * p.splits, sms / 2, kB200Pairs});

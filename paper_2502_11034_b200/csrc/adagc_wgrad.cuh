@@ -22,11 +22,12 @@
 // next.  Every wait is bounded; a block that gives up writes NaN over what it still owes.
 //
 // The tensor core cuts, not rounds, when it adds to an accumulator: measured against 64 bits, the relative error of a
-// gradient grows from 2e-7 (1024 tokens) over 1.1e-6 (4096) to 7e-6 (16384), and twice that where the tokens' scales differ.
-// An fp32 result therefore leaves the accumulator every 1536 tokens at most and is added up in fp32 with rounding; a bf16
-// result does not need that (8192 x 4096 x 11008, fp32 out: 567 us with 2816, 664 with 1536, 728 with 1024).  It is added up in
-// dW itself, or, if dW holds something to be added to, in a block of the workspace (750 to 790 us; adding each time to dW took 760
-// to 790 and rounded as often): the old values may be far above the sum, and are rounded onto once.
+// gradient grows from 2e-7 (1024 tokens) over 1.1e-6 (4096) to 7e-6 (16384), and twice that where the tokens' scales differ.  Where all
+// products have one sign it is 5e-5 at 16384 tokens, 3e-4 at 65536 and 1.6e-3 at 262144.
+// An fp32 result therefore leaves the accumulator every 1536 tokens at most and is added up in fp32 with rounding (8192 x 4096 x
+// 11008: 567 us with 2816, 664 with 1536, 728 with 1024), a bf16 result every 16384.  fp32 is added up in dW itself; bf16, and fp32 if
+// dW holds something to be added to, in a block of the workspace: the old values may be far above the sum, and are rounded onto
+// once (755 to 800 us; adding to dW at each exit took 760 to 810).
 #pragma once
 
 #include <cuda.h>
@@ -46,6 +47,7 @@ constexpr int kWgSmem = 1024 + kWgSlots * (kWgBytesA + kWgBytesB) + kWgSlotsCode
 constexpr int kWgAtom = 64 * kWgStep * 2;  // 64 features x 64 tokens of bf16: one swizzled column of a tile
 constexpr uint32_t kWgTmemCols = 512;
 constexpr int kWgExactSteps = 1536 / kWgStep;  // steps after which an fp32 result leaves the accumulator, at most
+constexpr int kWgLongSteps = 16384 / kWgStep;  // the same of a bf16 result
 
 // Instruction descriptor of tcgen05.mma kind::f16: fp32 accumulator, bf16 operands, both MN-major, M = 256, N = 256.
 constexpr uint32_t kWgInstr = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((kWgTileN / 8) << 17) | ((kWgPairK / 16) << 24);
@@ -182,9 +184,14 @@ __device__ __forceinline__ void wg_store(T* out, int64_t ld, int n, bool mine, u
   int left = mine ? min(n, kWgTileN) : 0;  // columns from `out` on
   float old[2][kCols];
   const auto fetch = [&](const T* p, int there, float (&o)[kCols]) {
+    if (there >= kCols) {  // (loads under a condition each can end up waiting for one another)
 #pragma unroll
-    for (int c = 0; c < kCols; ++c, p += ld)
-      if (c < there) o[c] = wg_load(p);
+      for (int c = 0; c < kCols; ++c, p += ld) o[c] = wg_load(p);
+    } else {
+#pragma unroll
+      for (int c = 0; c < kCols; ++c, p += ld)
+        if (c < there) o[c] = wg_load(p);
+    }
   };
   if constexpr (kAdd) {
     fetch(out, left, old[0]);
@@ -225,11 +232,11 @@ __device__ __forceinline__ void wg_store(T* out, int64_t ld, int n, bool mine, u
   }
 }
 
-// The end of a tile that is summed up apart from dW: the accumulator and `sums`, added, onto what `out` holds, in one rounding (one
-// addition per element: nothing depends on an order).  A reduction in place of a load and a store, because the usual paths leave no
-// registers for both: with loads here 8192 x 4096 x 11008 took 950 to 1280 us instead of 760.
-template <typename Arrived>
-__device__ __forceinline__ void wg_finish(float* out, int64_t ld, const float* sums, int n, uint32_t acc, const bool& ok, Arrived arrived) {
+// The end of a tile that is summed up apart from dW: the accumulator and `sums`, added, into `out`; onto what it holds for fp32, and
+// with `onto` for bf16; in one rounding.  fp32: a reduction (one addition per element: nothing depends on an order) in place of a load
+// and a store, because the usual paths leave no registers for both: with loads here 8192 x 4096 x 11008 took 950 us instead of 770.
+template <typename T, typename Arrived>
+__device__ __forceinline__ void wg_finish(T* out, int64_t ld, bool onto, const float* sums, int n, uint32_t acc, const bool& ok, Arrived arrived) {
   constexpr int kCols = 16;
   arrived();
 #pragma unroll 1
@@ -241,9 +248,27 @@ __device__ __forceinline__ void wg_finish(float* out, int64_t ld, const float* s
     __syncwarp();
     wg_tmem_load16(acc + c0, v);
     wg_tmem_wait(v);
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int c = 0; c < kCols; ++c, out += ld)
-      if (c0 + c < n) wg_add(out, ok ? __uint_as_float(v[c]) + sum[c] : quiet_nan());
+      for (int c = 0; c < kCols; ++c, out += ld)
+        if (c0 + c < n) wg_add(out, ok ? __uint_as_float(v[c]) + sum[c] : quiet_nan());
+    } else {
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) sum[c] = ok ? __uint_as_float(v[c]) + sum[c] : quiet_nan();
+      if (onto && c0 < n) {
+        const T* p = out;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          v[c] = *reinterpret_cast<const uint16_t*>(p);
+          if (c0 + c + 1 < n) p += ld;  // (beyond the last column that one again)
+        }
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) sum[c] += __uint_as_float(v[c] << 16);
+      }
+#pragma unroll
+      for (int c = 0; c < kCols; ++c, out += ld)
+        if (c0 + c < n) wg_put(out, sum[c]);
+    }
   }
 }
 
@@ -448,8 +473,10 @@ adagc_act8_wgrad_kernel(const __grid_constant__ CUtensorMap map_codes, const __g
       };
       const bool part = w.block >= 0, add = !first || (a.accumulate && !part);
       if (part && w.whole && last) {
-        wg_finish(static_cast<float*>(a.out) + w.n0 * a.ld_out + k, a.ld_out,
-                  a.partials + static_cast<int64_t>(w.block) * kWgTileN * kWgPairK + (rank * kWgTileK + quad * 32 + lane), k < a.k ? a.n - w.n0 : 0, acc, ok, arrived);
+        const float* sums = a.partials + static_cast<int64_t>(w.block) * kWgTileN * kWgPairK + (rank * kWgTileK + quad * 32 + lane);
+        const int n = k < a.k ? a.n - w.n0 : 0;
+        if (a.out_bf16) wg_finish(static_cast<__nv_bfloat16*>(a.out) + w.n0 * a.ld_out + k, a.ld_out, a.accumulate, sums, n, acc, ok, arrived);
+        else wg_finish(static_cast<float*>(a.out) + w.n0 * a.ld_out + k, a.ld_out, true, sums, n, acc, ok, arrived);
       } else if (part || !a.out_bf16) {
         float* out = part ? a.partials + static_cast<int64_t>(w.block) * kWgTileN * kWgPairK + (rank * kWgTileK + quad * 32 + lane)
                           : static_cast<float*>(a.out) + w.n0 * a.ld_out + k;

@@ -69,3 +69,24 @@ def test_fp32_accumulation_rounds_once_onto_what_is_there(n, k):
     act8.linear_wgrad(dy, x8, out=out, accumulate=True)
     off = (out.double() - (old.double() + alone.double())).abs().max()
     assert float(off) <= 2 ** -4 + 2 ** -20 * float(alone.abs().max())
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_bfloat16_result_over_many_tokens(accumulate):
+    """All products positive, the worst case for cutting: a chain of 16384 tokens loses at most 1024 * 2^-23 of the sum, the rounded
+    additions of 8 such chains (and of the old value) 9 * 2^-24; then one rounding to bfloat16, half an ulp.  Output features have scales
+    of their own, so that the results lie anywhere between two bfloat16 numbers."""
+    tokens, n, k = 1 << 17, 9224, 257                                               # 74 tiles, all whole
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 20 GB")
+    gen = torch.Generator("cuda").manual_seed(6)
+    scale = torch.rand(n, device="cuda", generator=gen) / 2 + 0.5
+    dy = torch.empty(tokens, n, dtype=torch.bfloat16, device="cuda")
+    for part in dy.split(1 << 15):
+        part.copy_((torch.rand(part.shape, device="cuda", generator=gen) + 0.5) * scale)
+    x8 = act8.encode((torch.rand(tokens, k, device="cuda", generator=gen) + 0.5).bfloat16())
+    old = (torch.rand(n, k, device="cuda", generator=gen) * 1e5).bfloat16() if accumulate else None
+    got = act8.linear_wgrad(dy, x8, torch.bfloat16, out=None if old is None else old.clone(), accumulate=accumulate)[:256].double()
+    want = dy[:, :256].double().T @ act8.decode(x8, torch.float32).double() + (0 if old is None else old[:256].double())
+    tol = torch.exp2(torch.floor(torch.log2(want)) - 8) + want * (1024 * 2 ** -23 + 9 * 2 ** -24)
+    assert float(((got - want).abs() / tol).max()) <= 1
