@@ -41,6 +41,8 @@ extern "C" {
  * fills hold index -1 and ln p = -inf.  A row with every entry masked: lse = -inf, logprob = -inf (0 without a target),
  * entropy = 0.  A row of equal finite values (the type's lowest among them) is uniform.  A row that holds a NaN or +inf
  * gives NaN in every output (but logprob 0 without a target) and -1 in every index.
+ * Masks cost time where they are scattered over a row: with a tenth of the entries at -inf at random, 8192 x 128256 bf16 takes
+ * about twice as long (fp32 a quarter longer); masked ends or long stretches cost little.
  */
 #define ADAGC_MAX_TOP_K 32
 int adagc_token_logprobs(const void* d_logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t ld,

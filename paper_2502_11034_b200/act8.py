@@ -8,7 +8,8 @@ Forward of a SwiGLU MLP:              Backward:
 
 x8, gate8 and up8 are all that is kept between the two: 3 + 3/32 bytes per element instead of 8 (bfloat16 x, gate, up, h).
 Calls only enqueue work, on `stream` (default: the current stream); outputs belong to that stream.  Tensors made or freed on
-another stream have to be ordered by the caller, as with every entry point of this package.
+another stream have to be ordered by the caller, as with every entry point of this package.  There is no autograd here: tensors
+that require a gradient are read (and written) as they are, results never require one, and the backward pass is calls of its own.
 """
 from __future__ import annotations
 

@@ -13,8 +13,8 @@
 //
 // What bounds it is shared memory: per step a block's copies and its decoding write 40 KB and read 8 KB there besides the
 // operands that the tensor core reads.  Hence two SMs work on one tile (cta_group::2): each keeps one half of both operands.
-// Large products then run into the power limit: 8192 x 4096 x 11008 takes 550 us in short runs (1343 TFLOP/s, tensor pipe 81 %
-// active) and 617 to 640 us back to back.
+// Large products then run into the power limit: 8192 x 4096 x 11008 takes 540 us in short runs (1368 TFLOP/s, tensor pipe 81 %
+// active) and 630 to 640 us back to back, at an SM clock of 1.28 GHz.
 //
 // Roles of a block's 16 warps: 0 copies the codes, 1 (of the pair's first block) issues the MMAs, 2 fetches the exponents,
 // 3 copies dY and owns the tensor memory, 4-7 epilogue, 8-15 decode.  The codes have a ring of their own, so that they are

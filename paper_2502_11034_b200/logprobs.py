@@ -5,14 +5,14 @@
     grad_logits = token_logprobs_backward(logits, targets, r.lse, r.entropy, grad_logprob=torch.full_like(r.logprob, -1 / n))
 
 Calls only enqueue work, on `stream` (default: the current stream); outputs belong to that stream.  Tensors made or freed on
-another stream have to be ordered by the caller, as with every entry point of this package.
+another stream have to be ordered by the caller, as with every entry point of this package.  There is no autograd here: tensors
+that require a gradient are read (and written) as they are, results never require one, and the backward pass is a call of its own.
 """
 from __future__ import annotations
 
 from typing import NamedTuple, Optional
 
 import torch
-
 
 from .binding import check, lib, matrix_args, run_on, vector_ptr
 
